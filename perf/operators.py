@@ -100,29 +100,22 @@ class State:
     pass
 
 
-_context = None
-
-
-def context():
-    """The program's one context of the library."""
-    global _context
-    if _context is None:
-        from paper_2409_13761_b200 import kdn
-        _context = kdn.kdn_create(0)
-    return _context
-
-
 class Handle:
-    """The library, its context and the pool it was told of."""
+    """A context of the library with the pool it was told of; gone with the state that keeps it."""
 
     def __init__(self, s, heads, dim, block, blocks):
         from paper_2409_13761_b200 import kdn
-        self.kdn, self.ctx = kdn, context()
+        self.kdn, self.ctx = kdn, kdn.kdn_create(0)
         if heads:
             half = s.pool.shape[0] // 2
             self.desc = kdn.pool_desc(half, heads, dim, block, blocks, [s.pool[2 * l].data_ptr() for l in range(half)],
                                       [s.pool[2 * l + 1].data_ptr() for l in range(half)])
             self.pool_id = kdn.kdn_pool_register(self.ctx, self.desc)
+
+    def __del__(self):
+        if getattr(self, "ctx", None) is not None:
+            self.kdn.kdn_destroy(self.ctx)
+            self.ctx = None
 
 
 def _gain(rng, heads, dim):
