@@ -91,6 +91,9 @@ __device__ __forceinline__ long long lse_at(const WeighLaunch &L, const WeighRec
 //     16      23 and 28 (13 and 12)      52 and 88 (37 and 41)      59 and 86 (35 and 39)
 // A given lse at 4 rows of 16 x 4096 tokens reads 134 MB of keys at 4.3 TB/s.
 constexpr int kFewRows = 16, kFewWarps = 8, kFewTokens = 32;     // tokens a warp's unit
+// The warps of a launch that have units.  Whoever joins the parts of a segment takes every worker between its first and its last to have left one, so that
+// there must be none without a unit.
+__host__ __device__ __forceinline__ unsigned few_workers(unsigned ctas, unsigned units) { return ctas * kFewWarps < units ? ctas * kFewWarps : units; }
 
 template <int D, int NB, bool GIVEN>
 __global__ void __launch_bounds__(kFewWarps * 32, 2) kdn_weigh_few_kernel(const __grid_constant__ WeighLaunch L)
@@ -101,10 +104,10 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) kdn_weigh_few_kernel(const 
     const WeighRec *recs = records(L);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const __nv_bfloat16 *pool = L.k_layers[L.layer];
-    const unsigned workers = gridDim.x * kFewWarps, me = blockIdx.x * kFewWarps + (unsigned)warp;
+    const unsigned workers = few_workers(gridDim.x, L.units), me = blockIdx.x * kFewWarps + (unsigned)warp;
+    if (me >= workers) return;
     // units are (record, head, tile of 32 tokens), tiles fastest; a warp is the worker
     const unsigned u0 = first_unit(me, L.units, workers), u1 = first_unit(me + 1, L.units, workers);
-    if (u0 == u1) return;
     int ri = record_of(recs, L.n, u0);
     WeighRec r = recs[ri];
     int h = (int)((u0 - r.unit) / (unsigned)r.tiles), tile = (int)((u0 - r.unit) % (unsigned)r.tiles);
@@ -859,7 +862,7 @@ kdn_status kdn_weigh(kdn_ctx *ctx, int pool_id, int layer, const kdn_weigh_req *
             if (ctas) st = d64 ? launch_few<64>(c, L, rows, given, ctas, stream) : launch_few<128>(c, L, rows, given, ctas, stream);
             if (st == KDN_OK && !given) {
                 const dim3 by_token((unsigned)(tokens ? (tokens + 1023) / 1024 : 1), (unsigned)L.H, by_row.z);
-                st = launch(c, rows <= 8 ? kdn_weigh_add_scores_kernel<8> : kdn_weigh_add_scores_kernel<16>, by_token, 256, 0, stream, L, ctas * kFewWarps);
+                st = launch(c, rows <= 8 ? kdn_weigh_add_scores_kernel<8> : kdn_weigh_add_scores_kernel<16>, by_token, 256, 0, stream, L, few_workers(ctas, L.units));
             }
         }
         if (st != KDN_OK) return st;
