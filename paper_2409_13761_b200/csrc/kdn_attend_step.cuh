@@ -319,8 +319,8 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
 
     // The queries, eight channels (of one word of codes) to four registers.  Codes in row groups: fp16 pairs (j, j + 4), all there is of a query
     // as it came, and in low_q what that leaves of one that was turned: 22 bits.  Codes in channel groups: fp32, four channels here and four
-    // there, times the power of two that brings the largest scale to about 1 (it moves when that has moved by 2^7); before each use times the scales of
-    // 64 tokens and then as two fp16 numbers too.
+    // there, times the power of two that brings the largest scale to about 1 (it moves when that has moved by 2^7, but by no more than leaves the queries,
+    // 2^8 at most, finite); before each use times the scales of 64 tokens and then as two fp16 numbers too.  A group whose scales are all zero moves nothing.
     uint32_t qa[8 * NG];
     float factor[2] = { 0.0f, 0.0f };
     int near = 127;                                         // codes in channel groups: the exponent that the largest scale has, or nearly
@@ -487,16 +487,15 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
                 float largest;
                 if (D == 128) {
                     const float4 y = *reinterpret_cast<const float4 *>(ks + 4 * lane);
-                    largest = fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w));
+                    largest = fmaxf(fmaxf(fabsf(y.x), fabsf(y.y)), fmaxf(fabsf(y.z), fabsf(y.w)));
                 } else {
                     const float2 y = *reinterpret_cast<const float2 *>(ks + 2 * lane);
-                    largest = fmaxf(y.x, y.y);
+                    largest = fmaxf(fabsf(y.x), fabsf(y.y));
                 }
-                const int e = min(max((int)__reduce_max_sync(0xffffffffu, __float_as_uint(fabsf(largest)) >> 23), 1), 253);
-                if (e > near + 6 || e < near - 6) {         // (a product is 2^15 at most, and what is lost of it 2^-25)
+                const int e0 = (int)__reduce_max_sync(0xffffffffu, __float_as_uint(largest) >> 23), e = min(max(e0, 8), 253);
+                if (e0 != 0 && (e > near + 6 || e < near - 6)) {         // (a product is 2^15 at most, and what is lost of it 2^-25)
                     const int half = (near - e) / 2, rest = near - e - half;
                     const float u0 = __uint_as_float((unsigned)(127 + half) << 23), u1 = __uint_as_float((unsigned)(127 + rest) << 23);
-                    const float d0 = __uint_as_float((unsigned)(127 - half) << 23), d1 = __uint_as_float((unsigned)(127 - rest) << 23);
                     auto moved = [&](uint32_t y) { return __float_as_uint(__uint_as_float(y) * u0 * u1); };
 #pragma unroll
                     for (int i = 0; i < 8 * NG; ++i) qa[i] = moved(qa[i]);
@@ -505,8 +504,6 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
                         const uint4 y = low_q[w * 32];
                         low_q[w * 32] = make_uint4(moved(y.x), moved(y.y), moved(y.z), moved(y.w));
                     }
-                    factor[0] = factor[0] * d0 * d1;
-                    factor[1] = factor[1] * d0 * d1;
                     near = e;
                 }
 #pragma unroll
@@ -537,10 +534,12 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
                         }
                     }
                 }
+                const float back = __uint_as_float((unsigned)near << 23);            // made anew for each tile: the factors keep their bits
+                const float by[2] = { factor[0] * back, factor[1] * back };
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[t][i] = acc[t][i] * factor[i % 2];
+                    for (int i = 0; i < 4; ++i) x[t][i] = acc[t][i] * by[i % 2];
             } else {
                 float acc[MT][NG][4];
                 auto products = [&](bool lower) {

@@ -72,3 +72,81 @@ def test_attend_reads_nothing_that_the_workspace_held(codec, n_q):
             c.call(workspace=torch.full((need,), 0xFF, dtype=torch.uint8, device=dev.dev)).check()
         finally:
             dev.close()
+
+
+# --------------------------------------------------------------------------- key scales far from 1 --
+
+def edit_scales(c, j, D, H, T, codec, keys=None, values=None):
+    """Part j of the first request: `keys` and `values` change the scales of the layer that is attended to, in place: [T][H][D/64], or keys in channel
+    groups [groups][H][D]."""
+    L, layer = c.dev.shape.n_layers, c.layer
+    buf = c.keep[j]
+    raw = buf.cpu().numpy()
+    scales = raw[L * 2 * (T * H * D // 2):].view(np.float32)
+    row = T * H * (D // 64)
+    per_key = -(-T // 64) * H * D if codec == KC64 else row
+    k0 = layer * (per_key + row)
+    k = scales[k0:k0 + per_key].reshape((-1, H, D) if codec == KC64 else (T, H, D // 64))
+    v = scales[k0 + per_key:k0 + per_key + row].reshape(T, H, D // 64)
+    if keys is not None:
+        keys(k)
+    if values is not None:
+        values(v)
+    buf.copy_(torch.from_numpy(raw))
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        planes = ref.decode(raw, L, H, D, T, codec == KC64, layer)
+    old = c.refs[0][3][j]
+    c.refs[0][3][j] = (planes[0], planes[1], old[2], old[3])
+
+
+GROUPS = {
+    "zero first": [0.0, 1.0, 1.0, 1.0],
+    "zero in the middle": [1.0, 0.0, 0.0, 1.0],
+    "zero last": [1.0, 1.0, 1.0, 0.0],
+    "all zero": [0.0, 0.0, 0.0, 0.0],
+    "tiny and back": [1.0, 1e-30, 1.0, 1e-10],
+    "smallest normal and back": [1.0, 2.0 ** -126 / 0.02, 0.0, 1.0],
+    "up": [1e-30, 1e-20, 1e-10, 1.0],
+}
+
+
+@pytest.mark.parametrize("what", GROUPS)
+@pytest.mark.parametrize("n_q", [1, 10, 11, 40])
+@pytest.mark.parametrize("D,H", [(64, 1), (64, 8), (128, 2), (128, 8)])
+def test_channel_groups_of_zero_and_far_scales(what, n_q, D, H):
+    """Keys in channel groups: a factor on all scales of a group of 64 tokens, for the even heads (the odd ones stay as they are)."""
+    T, codec = 64 * 3 + 50, KC64
+    dev = make_attend(H, D)
+    try:
+        rng = np.random.default_rng(D + H + n_q)
+        c = AttendCase(dev, rng, [(n_q, 500, [(T, codec, 7, 0), (T, codec, T, T)])], 4)
+
+        def keys(k):
+            k[:, ::2] *= np.array(GROUPS[what], dtype=np.float32)[:, None, None]
+
+        for j in range(2):
+            edit_scales(c, j, D, H, T, codec, keys=keys)
+        c.call().check()
+    finally:
+        dev.close()
+
+
+@pytest.mark.parametrize("n_q", [1, 10, 11])
+def test_a_chunk_of_keys_that_were_never_written(n_q):
+    """Stored by the library from a pool that holds zeros for 64 tokens and more."""
+    H, D, T = 2, 128, 300
+    dev = make_attend(H, D)
+    try:
+        rng = np.random.default_rng(3)
+        pool = ref.bits(rng.standard_normal((2, 2, 19, 16, H, D)))
+        pool[:, 0, 3:14] = 0
+        data = oracle.store(pool, np.arange(19, dtype=np.int32), 0, T, KC64)
+        c = AttendCase(dev, rng, [(n_q, 400, [(T, KC64, 0, 0)])], 4)
+        c.keep[0].copy_(torch.from_numpy(data))
+        k, v = ref.decode(data, 2, H, D, T, True, c.layer)
+        assert (k[64:192] == 0).all()
+        c.refs[0][3][0] = (k, v, 0, 0)
+        c.call().check()
+    finally:
+        dev.close()
