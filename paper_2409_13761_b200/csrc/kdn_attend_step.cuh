@@ -602,7 +602,8 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
                         if (tok >= n || tok > last1) x[t][2 * e + 1] = -INFINITY;
                     }
             }
-            // m follows the maximum only when that is 2^8 above it: weights stay below 2^8, and sums are seldom rescaled
+            // m follows the maximum only when that is 2^8 above it: weights stay below 2^8, and sums are seldom rescaled.  Each row for itself, so that
+            // no row's rounding goes by what another one sees.
             float top[2], base[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -615,8 +616,9 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
             if (__any_sync(0xffffffffu, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float a = top[j] == -INFINITY ? 0.0f : exp2_approx(m[j] - top[j]);
-                    m[j] = top[j];
+                    const bool move = top[j] > m[j] + 8.0f;
+                    const float a = move ? exp2_approx(m[j] - top[j]) : 1.0f;
+                    if (move) m[j] = top[j];
                     l[j] *= a;
 #pragma unroll
                     for (int i = 0; i < 4 * NG; ++i) { o[i][j] *= a; o[i][2 + j] *= a; }

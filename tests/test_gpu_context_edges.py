@@ -150,3 +150,59 @@ def test_a_chunk_of_keys_that_were_never_written(n_q):
         c.call().check()
     finally:
         dev.close()
+
+
+# ----------------------------------------------------------------- tokens that only some rows see --
+
+@pytest.mark.parametrize("value", [float("inf"), 1e20, 3e38, 1e4])
+@pytest.mark.parametrize("n_q,g,H", [(2, 4, 2), (2, 4, 8), (2, 1, 16)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scales_of_tokens_that_later_rows_see_do_not_matter(value, n_q, g, H, D):
+    """The key scales of the last token that is seen at all, by the last new token only, are huge or infinite: the rows before it keep their bits."""
+    T, codec = 80 + n_q + 100, G64
+    dev = make_attend(H, D)
+    try:
+        rng = np.random.default_rng(n_q + D)
+        c = AttendCase(dev, rng, [(n_q, 80, [(T, codec, 0, 0)])], g).call().check()
+        want, want_lse = c.out.clone(), c.lse.clone()
+
+        def keys(k):
+            k[80 + n_q - 1] = value
+
+        edit_scales(c, 0, D, H, T, codec, keys=keys)
+        c.call()
+        assert dev.sync() == 0
+        assert torch.equal(c.out[:-1], want[:-1]) and torch.equal(c.lse[:-1], want_lse[:-1])
+        if value < 1e30:                                                      # (products with 3e38 pass what 32 bits hold)
+            c.check()
+    finally:
+        dev.close()
+
+
+@pytest.mark.parametrize("value", [float("inf"), 1e4])
+@pytest.mark.parametrize("n_q", [2, 5])
+def test_a_row_rounds_by_what_it_sees_itself(value, n_q):
+    """The same with so many requests (over one chunk) that each is gone through tile by tile in one place; a token of the last of three tiles has some
+    rows move their reference but not the others."""
+    H, D, codec, seen = 8, 64, G64, 32 * 3 - 10
+    dev = make_attend(H, D, L=1)
+    try:
+        rng = np.random.default_rng(n_q)
+        c = AttendCase(dev, rng, [(n_q, seen - n_q, [(seen, codec, 0, 0)]) for _ in range(296)], 4, layer=0)
+        for r in c.recs:
+            r.parts = c.recs[0].parts
+        c.call()
+        assert dev.sync() == 0
+        want, want_lse = c.out.clone(), c.lse.clone()
+
+        def keys(k):
+            k[seen - 1] = value
+
+        edit_scales(c, 0, D, H, seen, codec, keys=keys)
+        c.call()
+        assert dev.sync() == 0
+        before = torch.arange(c.rows, device=dev.dev) % n_q != n_q - 1
+        assert torch.equal(c.out[before], want[before]) and torch.equal(c.lse[before], want_lse[before])
+        assert not torch.equal(c.lse[~before], want_lse[~before])
+    finally:
+        dev.close()
