@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) kdn_attend_block_kernel(cons
             // Two passes over the row's 64 scores, the second in a short loop that reads them again from tensor memory: code that stays in the
             // instruction cache and few registers are worth more than that read.
             const uint32_t s_col = s_base + (turns & 1u) * 64u;
-            const float scale = factor * sh.key_power[ring];
+            float scale = factor * sh.key_power[ring];
             float top = -INFINITY;
             auto maxima = [&](auto whole) {
                 uint32_t x[2][32];
@@ -275,6 +275,21 @@ __global__ void __launch_bounds__(kBlockThreads, 1) kdn_attend_block_kernel(cons
             if (all) maxima(std::true_type{});
             else maxima(std::false_type{});
             top *= scale;
+            // huge scores are multiplied and rounded before the reference is taken off
+            if (__any_sync(0xffffffffu, fabsf(top) > kHugeScore && fabsf(top) != INFINITY)) {
+                const float by = fabsf(top) > kHugeScore ? scale : 1.0f;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kBlockTile; c0 += 16) {
+                    uint32_t y[16];
+                    tc_load16(y, s_col + c0);
+                    tc_wait_loads();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * by);
+                    tc_store16(s_col + c0, y);
+                }
+                tc_wait_stores();
+                if (by != 1.0f) scale = 1.0f;
+            }
             // the reference follows the maximum when that is 2^8 above it
             const bool move = top > m + 8.0f;
             if (__any_sync(0xffffffffu, move)) {

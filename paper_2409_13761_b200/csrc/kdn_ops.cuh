@@ -138,6 +138,9 @@ __device__ __forceinline__ float exp2_approx(float x)       // 2 ulp, flushes re
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Kernels that take 2^(x * scale - m) in one multiply-add have rounded m (the largest x * scale) before: what that left is an exponent which all weights of the row
+// share, 2 at most with scores up to this (in powers of two).  Beyond, it would be a weight of infinity or none at all for the row's largest score, and x * scale is rounded first.
+constexpr float kHugeScore = 67108864.0f;                  // 2^26
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
 {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);

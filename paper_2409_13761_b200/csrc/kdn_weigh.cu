@@ -526,8 +526,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) kdn_weigh_many_kernel(const __g
                                 l *= exp2_approx(m - top);
                                 m = top;
                             }
+                            float by = L.scale;
+                            if (__any_sync(0xffffffffu, fabsf(top) > kHugeScore && fabsf(top) != INFINITY) && fabsf(top) > kHugeScore) {
+                                by = 1.0f;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * L.scale);
+                            }
                             const float base = m == -INFINITY ? 0.0f : -m;
-                            const f32x2 scale2 = pack2(L.scale, L.scale), base2 = pack2(base, base);
+                            const f32x2 scale2 = pack2(by, by), base2 = pack2(base, base);
                             f32x2 sum2 = pack2(0.0f, 0.0f);
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) {

@@ -108,6 +108,8 @@ GROUPS = {
     "tiny and back": [1.0, 1e-30, 1.0, 1e-10],
     "smallest normal and back": [1.0, 2.0 ** -126 / 0.02, 0.0, 1.0],
     "up": [1e-30, 1e-20, 1e-10, 1.0],
+    "huge and back": [1.0, 1e30, 1e-30, 1.0],
+    "down": [1e30, 1e10, 1.0, 1e-30],
 }
 
 
@@ -204,5 +206,46 @@ def test_a_row_rounds_by_what_it_sees_itself(value, n_q):
         before = torch.arange(c.rows, device=dev.dev) % n_q != n_q - 1
         assert torch.equal(c.out[before], want[before]) and torch.equal(c.lse[before], want_lse[before])
         assert not torch.equal(c.lse[~before], want_lse[~before])
+    finally:
+        dev.close()
+
+
+# ------------------------------------------------------------------------------------ huge scores --
+
+@pytest.mark.parametrize("gain", [1e6, 1e12, 1e25])
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_weigh_with_huge_scores(gain, n_q):
+    """The log-sum-exp of scores so large that one step of them in 32 bits is more than any weight's exponent (so that of the weights only this is sure:
+    they are numbers).  Bounds as for other scores: 136 * 2^-24 of sum |q k| for the sums, fp32's own step for the result."""
+    rng = np.random.default_rng(6)
+    c = WeighCase(rng, 2, 128, 4, 16, [(n_q, 300, 300)], q_gain=gain)
+    try:
+        c.call()
+        assert c.dev.sync() == 0
+        k = c.keys[c.tables[0][np.arange(300) // 16], np.arange(300) % 16]
+        add, want, reach = ref.weigh(c.q64, k, 300, c.scale)
+        assert (np.abs(c.lse.cpu().numpy().astype(np.float64) - want) <= 2.0 ** -16.9 * reach + 2.0 ** -18 + 2.0 ** -22 * np.abs(want)).all()
+        assert not torch.isnan(c.acc[0]).any()
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("gain", [1e6, 1e12, 1e25])
+@pytest.mark.parametrize("codec", [G64, KC64])
+@pytest.mark.parametrize("n_q", [1, 11, 70])
+def test_attend_with_huge_scores(gain, codec, n_q):
+    """One row's queries are huge, the others' are not: those keep their bits."""
+    dev = make_attend(2, 128)
+    try:
+        rng = np.random.default_rng(7)
+        c = AttendCase(dev, rng, [(n_q, 400, [(200, codec, 7, 0), (150, codec, 0, 200)])], 4).call().check()
+        want, want_lse = c.out.clone(), c.lse.clone()
+        c.q[n_q // 2, 5] *= gain
+        c.q64[n_q // 2, 5] = c.q[n_q // 2, 5].double().cpu().numpy()
+        c.call().check()
+        assert torch.isfinite(c.out).all() and torch.isfinite(c.lse).all()
+        rest = torch.ones_like(c.lse, dtype=torch.bool)
+        rest[n_q // 2, 5] = False
+        assert torch.equal(c.out[rest], want[rest]) and torch.equal(c.lse[rest], want_lse[rest])
     finally:
         dev.close()
