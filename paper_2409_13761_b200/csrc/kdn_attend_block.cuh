@@ -3,8 +3,9 @@
 // Mathematics as for a few (kdn_attend_step.cuh), other places for the scales.  Rows of queries are the lanes of tensor memory, 64 tokens of a tile its
 // columns:  S = Q K^T with K = code * scale as the sum of two fp16 matrices (scale = two numbers of eight bits, whose products with a code are exact) and
 // Q, turned and times a power of two, as the sum of two more (the second is nothing, and left out, where the queries are taken as they came);  P = exp(S) *
-// value scale, bf16, one matrix for each group of 64 channels;  O += P C with C the value codes, exact in bf16.  The keys of a tile are held times the
-// power of two that brings the largest of their scales to 1.  P is rounded once (2^-9 relative): tensor memory has no room for a second number, and fp16 not the
+// value scale, bf16, one matrix for each group of 64 channels;  O += P C with C the value codes, exact in bf16.  The keys of a tile are held times a
+// power of two that brings the largest of their scales to 2^11, or, where scales are more than 2^12 apart, each token's times one of its own, which its
+// column of S is multiplied by before the softmax.  P is rounded once (2^-9 relative): tensor memory has no room for a second number, and fp16 not the
 // range that scales need; the result is 1.4 to 1.5 times as far off (root mean square, against 64 bits) as its own rounding alone makes it.
 //
 // What bounds it: shared memory's 128 bytes a clock, at about four fifths.  A tile of 64 tokens by 256 rows takes some 4000 clocks, of which the operands of the products
@@ -35,7 +36,9 @@ struct BlockShared {
     unsigned long long k_full[2], k_empty[2], v_full, v_empty, q_full[2], s_full[2][2], p_full[2][2], o_full[2], drained;
     uint32_t tmem;
     volatile int abort_flag;
-    float value_scale[4][2][kBlockTile], key_power[4];                    // of the tiles under way, by tile number modulo 4
+    // Of the tiles under way, by tile number modulo 4.  key_power: what the tile's keys were divided by, or 0 where each token's were divided by a power
+    // of its own (key_column).
+    float value_scale[4][2][kBlockTile], key_power[4], key_column[4][kBlockTile];
     float2 table[8][64];                                                  // rotation of the part, for each softmax warp
     uint32_t channel[4][2][32];                                           // codes in channel groups: a warp's 64 channels' scales, leading and rest
 };
@@ -116,6 +119,15 @@ __device__ __forceinline__ void powers_of(float a, float &down, float &up)
     e = e < 2 ? 2 : e > 252 ? 252 : e;
     down = __uint_as_float((unsigned)(254 - e) << 23);
     up = __uint_as_float((unsigned)e << 23);
+}
+// Powers of two that bring a scale of exponent field e (at least kLeastKey counts) to 2^kKeyTop and over, and back: times a code of 8 it is below 2^15 in fp16, and 2^-12
+// of it still has all the bits of an fp32 scale above fp16's smallest step, 2^-24.
+constexpr int kKeyTop = 11, kKeySpread = 12, kLeastKey = 14;
+__device__ __forceinline__ void key_powers(int e, float &down, float &up)
+{
+    e = e < kLeastKey ? kLeastKey : e > 254 ? 254 : e;
+    down = __uint_as_float((unsigned)(254 + kKeyTop - e) << 23);
+    up = __uint_as_float((unsigned)(e - kKeyTop) << 23);
 }
 
 template <int D>
@@ -255,7 +267,20 @@ __global__ void __launch_bounds__(kBlockThreads, 1) kdn_attend_block_kernel(cons
             // Two passes over the row's 64 scores, the second in a short loop that reads them again from tensor memory: code that stays in the
             // instruction cache and few registers are worth more than that read.
             const uint32_t s_col = s_base + (turns & 1u) * 64u;
-            float scale = factor * sh.key_power[ring];
+            const float power = sh.key_power[ring];
+            if (power == 0.0f) {                                 // a power of two for each token's scores
+#pragma unroll 1
+                for (int c0 = 0; c0 < kBlockTile; c0 += 16) {
+                    uint32_t y[16];
+                    tc_load16(y, s_col + c0);
+                    tc_wait_loads();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * sh.key_column[ring][c0 + i]);
+                    tc_store16(s_col + c0, y);
+                }
+                tc_wait_stores();
+            }
+            float scale = power == 0.0f ? factor : factor * power;
             float top = -INFINITY;
             auto maxima = [&](auto whole) {
                 uint32_t x[2][32];
@@ -500,14 +525,29 @@ __global__ void __launch_bounds__(kBlockThreads, 1) kdn_attend_block_kernel(cons
             const unsigned ring = i & 3u;
             // keys of tile i, then values of the one before, whose place is left later
             if (u < u1) {
-            float down, up;
-            float hi = 0.0f, lo = 0.0f, most = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 2 * NG; ++j) most = fmaxf(most, near[j]);
+            float down, up, column = 0.0f;
+            float hi = 0.0f, lo = 0.0f;
             if (NG == 2 && G) { cs[0] = near[2 * NG - 2]; cs[1] = near[2 * NG - 1]; }
             else { cs[0] = near[0]; cs[1] = near[1]; }
-            for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-            powers_of(most, down, up);
+            // Exponents of the tile's scales.  Where they are few apart, all keys are divided by one power of two; else, and where some are infinite, each token's by its own.  Both
+            // give a token's scores the same bits, so that no row's go by tokens that it does not see.
+            int e_max = 0, e_min = 255;
+#pragma unroll
+            for (int j = 0; j < 2 * NG; ++j) {
+                const int e = (int)(__float_as_uint(near[j]) >> 23 & 255u);
+                e_max = max(e_max, e);
+                if (e > 0) e_min = min(e_min, e);
+            }
+            e_max = __reduce_max_sync(0xffffffffu, e_max);
+            e_min = __reduce_min_sync(0xffffffffu, e_min);
+            key_powers(e_max, down, up);
+            if (!group_keys && e_max > 0 && (e_max == 255 || e_max - e_min > kKeySpread)) {
+                int e = 0;                                       // of this thread's token
+#pragma unroll
+                for (int j = 0; j < NG; ++j) e = max(e, (int)(__float_as_uint(t < 32 ? near[j] : near[NG + j]) >> 23 & 255u));
+                key_powers(e, down, column);
+                up = 0.0f;
+            }
             const bool by_channel = group_keys;
             if (by_channel) {
                 float h0, l0, h1, l1;
@@ -545,6 +585,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) kdn_attend_block_kernel(cons
                 }
             }
             if (me == 0) sh.key_power[ring] = up;
+            if (up == 0.0f && me < kBlockTile) sh.key_column[ring][t] = column;
             if (D == 128 || side == 0) sh.value_scale[ring][G][t] = vs;
             fence_async_smem();
             mbar_arrive(smem_u32(&sh.k_full[b]));

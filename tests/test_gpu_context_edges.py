@@ -157,7 +157,7 @@ def test_a_chunk_of_keys_that_were_never_written(n_q):
 # ----------------------------------------------------------------- tokens that only some rows see --
 
 @pytest.mark.parametrize("value", [float("inf"), 1e20, 3e38, 1e4])
-@pytest.mark.parametrize("n_q,g,H", [(2, 4, 2), (2, 4, 8), (2, 1, 16)])
+@pytest.mark.parametrize("n_q,g,H", [(2, 4, 2), (2, 4, 8), (2, 1, 16), (3, 16, 2), (40, 4, 2), (300, 1, 2)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_scales_of_tokens_that_later_rows_see_do_not_matter(value, n_q, g, H, D):
     """The key scales of the last token that is seen at all, by the last new token only, are huge or infinite: the rows before it keep their bits."""
@@ -206,6 +206,46 @@ def test_a_row_rounds_by_what_it_sees_itself(value, n_q):
         before = torch.arange(c.rows, device=dev.dev) % n_q != n_q - 1
         assert torch.equal(c.out[before], want[before]) and torch.equal(c.lse[before], want_lse[before])
         assert not torch.equal(c.lse[~before], want_lse[~before])
+    finally:
+        dev.close()
+
+
+@pytest.mark.parametrize("n_q,g", [(10, 4), (33, 4), (200, 1)])
+@pytest.mark.parametrize("D,turn", [(64, 0), (128, 0), (128, 9)])
+def test_each_row_has_the_precision_of_what_it_sees(n_q, g, D, turn):
+    """Key scales that grow from token to token, so that a row's largest score is far below those of the tile's other rows."""
+    H, T, codec = 2, 30 + n_q, G64
+    dev = make_attend(H, D)
+    try:
+        rng = np.random.default_rng(n_q)
+        c = AttendCase(dev, rng, [(n_q, 30, [(T, codec, turn, 0)])], g)
+
+        def keys(k):
+            k[30:] *= (8.0 ** np.minimum(np.arange(n_q), 30))[:, None, None].astype(np.float32)
+
+        edit_scales(c, 0, D, H, T, codec, keys=keys)
+        c.call().check()
+    finally:
+        dev.close()
+
+
+@pytest.mark.parametrize("n_q", [10, 11, 70])
+@pytest.mark.parametrize("D,turn", [(64, 5), (128, 0), (128, 5)])
+def test_key_scales_of_many_magnitudes(n_q, D, turn):
+    """Tokens and groups of channels over eight orders of magnitude, zero among them; parts of one and of many magnitudes in turn."""
+    H, T, codec = 2, 333, G64
+    dev = make_attend(H, D)
+    try:
+        rng = np.random.default_rng(n_q + D)
+        c = AttendCase(dev, rng, [(n_q, 1000, [(T, codec, turn, 0), (T, codec, T, T), (T, codec, 2 * T + turn, 2 * T)])], 4)
+
+        def keys(k):
+            k *= (10.0 ** rng.uniform(-8, 0, k.shape)).astype(np.float32)
+            k[rng.random(T) < 0.1] = 0.0
+
+        edit_scales(c, 1, D, H, T, codec, keys=keys)
+        edit_scales(c, 2, D, H, T, codec, keys=keys)
+        c.call().check()
     finally:
         dev.close()
 
