@@ -591,15 +591,17 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
                         }
                     }
             }
+            int last0 = 0, last1 = 0;                           // last tokens that the two rows see
             if (!full_tile) {
-                const int last0 = now.w + (seg.row0 + 2 * c) / L.g, last1 = now.w + (seg.row0 + 2 * c + 1) / L.g;
+                last0 = min(n - 1, now.w + (seg.row0 + 2 * c) / L.g);
+                last1 = min(n - 1, now.w + (seg.row0 + 2 * c + 1) / L.g);
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int tok = 16 * t + 8 * e + g;
-                        if (tok >= n || tok > last0) x[t][2 * e] = -INFINITY;
-                        if (tok >= n || tok > last1) x[t][2 * e + 1] = -INFINITY;
+                        if (tok > last0) x[t][2 * e] = -INFINITY;
+                        if (tok > last1) x[t][2 * e + 1] = -INFINITY;
                     }
             }
             // m follows the maximum only when that is 2^8 above it: weights stay below 2^8, and sums are seldom rescaled.  Each row for itself, so that
@@ -654,8 +656,8 @@ __global__ void __launch_bounds__(256, 2) kdn_attend_step_kernel(const __grid_co
                         for (int G = 0; G < NG; ++G) {
                             float p0 = x[t][2 * e] * s[G], p1 = x[t][2 * e + 1] * s[G];
                             if (!all) {                     // what is not seen may hold anything
-                                p0 = x[t][2 * e] == 0.0f ? 0.0f : p0;
-                                p1 = x[t][2 * e + 1] == 0.0f ? 0.0f : p1;
+                                if (16 * t + 8 * e + g > last0) p0 = 0.0f;
+                                if (16 * t + 8 * e + g > last1) p1 = 0.0f;
                             }
                             split_bf16x2(p0, p1, pw[t][G][e], pl[t][G][e]);
                         }

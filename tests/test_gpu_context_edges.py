@@ -289,3 +289,36 @@ def test_attend_with_huge_scores(gain, codec, n_q):
         assert torch.equal(c.out[rest], want[rest]) and torch.equal(c.lse[rest], want_lse[rest])
     finally:
         dev.close()
+
+
+# ------------------------------------------------------------------------------- NaN that is seen --
+
+@pytest.mark.parametrize("codec", [G64, KC64])
+@pytest.mark.parametrize("n_q", [1, 40])
+@pytest.mark.parametrize("T", [20, 64, 200])
+def test_nan_in_a_value_shows_however_small_its_weight(codec, n_q, T):
+    """A token whose weight is below what fp32 holds has a NaN for a value scale: the rows that see it are NaN, their lse is not."""
+    H, D, bad = 2, 128, 5
+    dev = make_attend(H, D)
+    try:
+        rng = np.random.default_rng(T)
+        c = AttendCase(dev, rng, [(n_q, T + 5, [(T, codec, 0, 0)])], 4, q_gain=400.0)
+        raw = c.keep[0].cpu().numpy()
+        row = H * D // 2
+        at = 2 * c.layer * T * row + bad * row
+        raw[at:at + row] = 0                                                  # a key of zeros: its score is 0, the largest some hundreds
+        c.keep[0].copy_(torch.from_numpy(raw))
+        edit_scales(c, 0, D, H, T, codec)
+        c.call().check()
+        assert (c.lse > 100.0).all()                                          # e^-100 is 2^-144
+        want_lse = c.lse.clone()
+
+        def values(v):
+            v[bad] = np.nan
+
+        edit_scales(c, 0, D, H, T, codec, values=values)
+        c.call()
+        assert dev.sync() == 0
+        assert torch.isnan(c.out).all() and torch.equal(c.lse, want_lse)
+    finally:
+        dev.close()
