@@ -179,14 +179,21 @@ __device__ __forceinline__ float max_or_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
-// 2^x of two numbers on the pipe of multiplications, for kernels that the special-function unit (16 results a clock and SM) holds up: 2^n 2^f with n the
+__device__ __forceinline__ float min_or_nan(float a, float b)
+{
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+// Half of 2^x of two numbers on the pipe of multiplications, for kernels that the special-function unit (16 results a clock and SM) holds up: 2^(n - 1) 2^f with n the
 // nearest whole number and 2^f by the polynomial of degree five through its values at the Chebyshev nodes of [-1/2, 1/2], off by 2.2e-7 relative at most in
-// fp32 (2^-22; worked out for these coefficients).  x below -126 counts as -126 and has to be below 128; a NaN stays one.
-__device__ __forceinline__ f32x2 exp2_pair(f32x2 x)
+// fp32 (2^-22; worked out for these coefficients).  Halves, so that every result that fp32 holds is made without overflow; whoever adds them up doubles
+// them in the same step, which gives infinity from x = 128 on.  Below x = -125.5 the result is zero; a NaN stays one.
+__device__ __forceinline__ f32x2 half_exp2_pair(f32x2 x)
 {
     float a, b;
     unpack2(x, a, b);
-    x = pack2(max_or_nan(a, -126.0f), max_or_nan(b, -126.0f));
+    x = pack2(min_or_nan(max_or_nan(a, -126.0f), 128.0f), min_or_nan(max_or_nan(b, -126.0f), 128.0f));
     const f32x2 whole = add2(x, pack2(12582912.0f, 12582912.0f));              // 1.5 * 2^23: n in the low bits
     const f32x2 f = fma2(add2(whole, pack2(-12582912.0f, -12582912.0f)), pack2(-1.0f, -1.0f), x);
     f32x2 y = pack2(0.0013390863314270973f, 0.0013390863314270973f);
@@ -197,7 +204,7 @@ __device__ __forceinline__ f32x2 exp2_pair(f32x2 x)
     y = fma2(y, f, pack2(1.0000001192092896f, 1.0000001192092896f));
     float n0, n1;
     unpack2(whole, n0, n1);
-    return mul2(y, pack2(__uint_as_float((__float_as_uint(n0) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(n1) << 23) + 0x3f800000u)));
+    return mul2(y, pack2(__uint_as_float((__float_as_uint(n0) << 23) + 0x3f000000u), __uint_as_float((__float_as_uint(n1) << 23) + 0x3f000000u)));
 }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

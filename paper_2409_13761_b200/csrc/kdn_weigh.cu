@@ -295,8 +295,8 @@ template <int ROWS> __global__ void __launch_bounds__(256) kdn_weigh_add_scores_
 // them at 16 a clock and SM, against rows * tokens * D / 4096 clocks of the products.  Two passes, each laid out so that a thread sums what it holds and no
 // thread needs another's: for the lse the rows are the lanes of tensor memory and the tokens its columns, for the weights the other way round.  K is
 // read by both (the second time mostly from L2).  Measured, 8 heads of 128 with 4 query heads each: 64 tokens of eight requests over 8209 tokens with the lse
-// given 75 us (0.46 PFLOP/s; its exponentials alone 30 us at 16 a clock); 32 tokens over 10272, lse to be found, 30 us: five tiles a CTA, so the chain from
-// the launch to the first scores counts twice.  12 of 32 exponentials of a full block go over the multipliers.
+// given 73 us (0.47 PFLOP/s; its exponentials alone 30 us at 16 a clock); 32 tokens over 10272, lse to be found, 30 us: five tiles a CTA, so the chain from
+// the launch to the first scores counts twice.  8 of 32 exponentials of a full block go over the multipliers (12: 77 us).
 //
 // Warps 0-3 copy keys and queries (asynchronous 16-byte copies, a fence to the tensor core's proxy), warp 4 issues the products, warps 5-8 and 9-12 take
 // the tiles in turn, each with two buffers of 128 columns.
@@ -572,9 +572,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) kdn_weigh_many_kernel(const __g
                                     const float4 v = ls[i];
                                     const f32x2 a = fma2(pack2(__uint_as_float(x[4 * i]), __uint_as_float(x[4 * i + 1])), scale2, pack2(v.x, v.y));
                                     const f32x2 b = fma2(pack2(__uint_as_float(x[4 * i + 2]), __uint_as_float(x[4 * i + 3])), scale2, pack2(v.z, v.w));
-                                    if (i % 8 == 1 || i % 8 == 4 || i % 8 == 6) {        // 12 of 32 beside the special-function unit
-                                        sum2 = add2(sum2, exp2_pair(a));
-                                        sum2 = add2(sum2, exp2_pair(b));
+                                    if (i % 8 == 2 || i % 8 == 6) {        // 8 of 32 beside the special-function unit
+                                        sum2 = fma2(half_exp2_pair(a), pack2(2.0f, 2.0f), sum2);
+                                        sum2 = fma2(half_exp2_pair(b), pack2(2.0f, 2.0f), sum2);
                                     } else {
                                         float e0, e1, e2, e3;
                                         unpack2(a, e0, e1);

@@ -322,3 +322,34 @@ def test_nan_in_a_value_shows_however_small_its_weight(codec, n_q, T):
         assert torch.isnan(c.out).all() and torch.equal(c.lse, want_lse)
     finally:
         dev.close()
+
+
+# --------------------------------------------------------------- a given lse far below the scores --
+
+@pytest.mark.parametrize("below", [60.0, 88.5, 89.0, 100.0, 1000.0])
+def test_given_lse_far_below_the_scores(below):
+    """Weights near and past what fp32 holds, from each place of a full block of 128 rows in turn.  A power's argument of up to 2^10.6 is rounded twice in 32 bits,
+    2^-14 of the result at most, and the power itself to 2^-21."""
+    rng = np.random.default_rng(8)
+    H = 8
+    c = WeighCase(rng, H, 64, 1, 16, [(128, 400, 256)], q_gain=1e-3)
+    try:
+        k = c.keys[c.tables[0][np.arange(256) // 16], np.arange(256) % 16]
+        score = c.scale * np.einsum("rhd,thd->rht", c.q64, k)
+        for first in range(0, 128, H):
+            lse = np.full((128, H), np.float32(np.log(256.0)))
+            odd = [first + h for h in range(H)]                               # a row for each head
+            lse[odd, range(H)] = -below
+            c.lse.copy_(torch.from_numpy(lse))
+            c.acc[0].copy_(torch.from_numpy(c.acc0[0]))
+            c.call(given=True)
+            assert c.dev.sync() == 0
+            with np.errstate(over="ignore"):
+                want = np.exp(score - lse.astype(np.float64)[:, :, None]).sum(0) + c.acc0[0][:, :256]
+            got = c.acc[0].cpu().numpy()[:, :256].astype(np.float64)
+            past = want > np.finfo(np.float32).max
+            assert (past == (below > 88.8)).all()
+            assert (got[past] == np.inf).all(), got[past]
+            assert (np.abs(got[~past] - want[~past]) <= 2.0 ** -13 * want[~past]).all()
+    finally:
+        c.close()
