@@ -426,7 +426,7 @@ typedef struct {
     int32_t     n_q_heads;
     int32_t     rope_style;     /* 0 = pairs (i, i + head_dim/2); no other style is implemented */
     double      rope_theta;     /* read where a part stands elsewhere than its base_pos */
-    double      scale;          /* of the scores, > 0 (1/sqrt(head_dim) in most models) */
+    double      scale;          /* of the scores, > 0 (1/sqrt(head_dim) in most models); scale * log2(e) in fp32 is neither 0 nor infinite */
     void       *workspace;
     size_t      workspace_bytes;
 } kdn_attend_io;
@@ -466,7 +466,7 @@ typedef struct {
     int64_t     q_stride;
     int32_t     n_q_heads;
     int32_t     lse_given;
-    double      scale;
+    double      scale;              /* as in kdn_attend_io */
     void       *workspace;
     size_t      workspace_bytes;
 } kdn_weigh_io;

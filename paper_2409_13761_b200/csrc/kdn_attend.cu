@@ -141,7 +141,7 @@ kdn_status kdn_validate_attend(const kdn_pool_desc *pool, int layer, const kdn_a
     const kdn_status st = check_reqs(pool, reqs, n_reqs, io->n_q_heads, &moved);
     if (st != KDN_OK) return st;
     if (layer < 0 || layer >= pool->n_layers) return KDN_E_INVAL;
-    if (!(io->scale > 0.0) || !std::isfinite((float)io->scale)) return KDN_E_INVAL;
+    if (!usable_scale(io->scale)) return KDN_E_INVAL;
     if (io->rope_style != 0) return KDN_E_UNSUPPORTED;
     if (moved && (!(io->rope_theta > 0.0) || io->rope_theta > 1e300)) return KDN_E_INVAL;
     int64_t rows = 0;
@@ -194,7 +194,7 @@ kdn_status kdn_attend(kdn_ctx *ctx, int pool_id, int layer, const kdn_attend_req
     L.q_stride = io->q_stride;
     L.out_stride = io->out_stride;
     L.wait_limit_ns = c.wait_limit_ns;
-    L.scale = (float)(io->scale * 1.4426950408889634);
+    L.scale = (float)(io->scale * kLog2e);
     L.H = H;
     L.g = g;
     L.bits = Bits{ 0x000f000fu, 0x43084308u, 0x64086408u, 0x00f000f0u, 0x64806480u, 0x2c002c00u, 0xd480d480u };

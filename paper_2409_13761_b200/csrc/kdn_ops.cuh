@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstring>
 
 #define KDN_CUDA(call)                                                                  \
@@ -54,6 +55,10 @@ template <auto kernel> kdn_status allow_smem(const Context &c, size_t bytes)
     done.fetch_or(bit, std::memory_order_relaxed);
     return KDN_OK;
 }
+
+constexpr double kLog2e = 1.4426950408889634;
+// Whether the kernels' scores, in powers of two, can be had from a scale: fp32 holds what they are multiplied by.
+inline bool usable_scale(double scale) { return (float)(scale * kLog2e) > 0.0f && std::isfinite((float)(scale * kLog2e)); }
 
 // Tokens of one request or chunk at most: what the kernels add to a token's index stays within 31 bits.
 constexpr int64_t kMostTokens = (int64_t)1 << 28;

@@ -2,7 +2,6 @@
 #include "kdn_ops.cuh"
 #include "kdn_tc.cuh"
 
-#include <cmath>
 #include <new>
 #include <vector>
 
@@ -758,7 +757,7 @@ kdn_status kdn_validate_weigh(const kdn_pool_desc *pool, int layer, const kdn_we
     const kdn_status st = check_reqs(pool, reqs, n_reqs, io->n_q_heads);
     if (st != KDN_OK) return st;
     if (layer < 0 || layer >= pool->n_layers) return KDN_E_INVAL;
-    if (!(io->scale > 0.0) || !std::isfinite((float)io->scale)) return KDN_E_INVAL;
+    if (!usable_scale(io->scale)) return KDN_E_INVAL;
     int64_t rows = 0;
     for (int i = 0; i < n_reqs; ++i) rows += reqs[i].n_q;
     if (rows == 0) return KDN_OK;
@@ -802,7 +801,7 @@ kdn_status kdn_weigh(kdn_ctx *ctx, int pool_id, int layer, const kdn_weigh_req *
     L.n_blocks = pool.desc.n_blocks;
     L.wait_limit_ns = c.wait_limit_ns;
     L.status = c.status;
-    L.scale = (float)(io->scale * 1.4426950408889634);
+    L.scale = (float)(io->scale * kLog2e);
     L.layer = layer;
     L.H = pool.desc.n_kv_heads;
     L.g = io->n_q_heads / L.H;

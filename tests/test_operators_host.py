@@ -128,6 +128,14 @@ def test_sizes_past_the_limits_are_refused():
     assert evict(n_tokens=most + 1, row_stride=most + 1) == uns and evict(n_rows=most + 1) == uns
 
 
+def test_scales_that_fp32_does_not_hold_are_refused():
+    """The kernels work in powers of two: what they multiply by is scale * log2(e) in fp32."""
+    for scale in (1e-46, 2.4e38, 3.4e38, 1e-300):
+        assert attend(scale=scale) == K.KDN_E_INVAL and weigh(scale=scale) == K.KDN_E_INVAL
+    for scale in (1e-38, 1.0, 2.3e38):
+        assert attend(scale=scale) == K.KDN_OK and weigh(scale=scale) == K.KDN_OK
+
+
 def test_calls_without_a_context_are_refused():
     arr = K.attend_array([])
     assert K.lib.kdn_attend(None, 0, 0, arr, 0, None, None) == K.KDN_E_INVAL
