@@ -376,6 +376,10 @@ def kdn_create(device: int = 0) -> C.c_void_p:
 
 def kdn_destroy(ctx) -> None:
     lib.kdn_destroy(ctx)
+    at = getattr(ctx, "value", ctx)                   # another context may come to lie there
+    for key in list(_pool_dims):
+        if key[0] == at:
+            del _pool_dims[key]
 
 
 def kdn_pool_register(ctx, desc: kdn_pool_desc) -> int:

@@ -353,3 +353,14 @@ def test_given_lse_far_below_the_scores(below):
             assert (np.abs(got[~past] - want[~past]) <= 2.0 ** -13 * want[~past]).all()
     finally:
         c.close()
+
+
+# -------------------------------------------------------------------------------------- bookkeeping --
+
+def test_a_destroyed_context_leaves_no_pools():
+    """Row strides that are left out go by the pools of the context at hand."""
+    dev = make_attend(2, 64)
+    K, at = dev.K, dev.ctx.value
+    assert K._head_dim(dev.ctx, dev.pool_id) == 64
+    dev.close()
+    assert not [k for k in K._pool_dims if k[0] == at]
