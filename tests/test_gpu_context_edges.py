@@ -324,6 +324,41 @@ def test_nan_in_a_value_shows_however_small_its_weight(codec, n_q, T):
         dev.close()
 
 
+@pytest.mark.parametrize("codec", [G64, KC64])
+@pytest.mark.parametrize("n_q", [8, 40])
+@pytest.mark.parametrize("plane", [0, 1])
+def test_infinities_that_were_stored(codec, n_q, plane):
+    """An infinite key or value leaves an infinite scale and zero codes in a chunk, whose product is no number: rows that see it are NaN, the others keep their bits."""
+    H, D, T, bad = 2, 128, 200, 64                                            # (keys in channel groups: the first token of a group)
+    dev = make_attend(H, D)
+    try:
+        rng = np.random.default_rng(12)
+        x = rng.standard_normal((2, 2, 13, 16, H, D)).astype(np.float32)
+        c = AttendCase(dev, rng, [(n_q, bad - 4, [(T, codec, 0, 0)])], 4)
+
+        def put(y):
+            data = oracle.store(ref.bits(y), np.arange(13, dtype=np.int32), 0, T, codec)
+            c.keep[0].copy_(torch.from_numpy(data))
+            with np.errstate(invalid="ignore"):
+                k, v = ref.decode(data, 2, H, D, T, codec == KC64, c.layer)
+            c.refs[0][3][0] = (k, v, 0, 0)
+            c.call()
+            return np.isnan((k, v)[plane][bad]).any()
+
+        assert not put(x)
+        c.check()
+        want, want_lse = c.out.clone(), c.lse.clone()
+        x[c.layer, plane, bad // 16, bad % 16, :, 5] = np.inf
+        assert put(x)
+        assert dev.sync() == 0
+        assert torch.equal(c.out[:4], want[:4]) and torch.equal(c.lse[:4], want_lse[:4])
+        # a key: the row; a value: the channels of its group of 64
+        assert torch.isnan(c.out[4:, :, :64]).all()
+        assert torch.isnan(c.lse[4:]).all() if plane == 0 else torch.isfinite(c.lse).all()
+    finally:
+        dev.close()
+
+
 # --------------------------------------------------------------- a given lse far below the scores --
 
 @pytest.mark.parametrize("below", [60.0, 88.5, 89.0, 100.0, 1000.0])
