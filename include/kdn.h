@@ -399,12 +399,13 @@ kdn_status kdn_compose_select(kdn_ctx *ctx, int pool_id, const kdn_compose_req *
  * graphs that may run at the same time were captured with workspaces of their own).  Queries, outputs, weights and
  * workspaces lie on the context's device.  Outputs overlap neither inputs nor one another.  A request or chunk has up to
  * 2^28 tokens, and kdn_evict's as many rows (KDN_E_UNSUPPORTED).  A call that is refused enqueues nothing.  NaN that a row reads (in its query, in a scale or a key that
- * it sees) makes that row's results NaN, and with kdn_weigh what the row adds. */
+ * it sees) makes that row's results NaN, and with kdn_weigh what the row adds.  Scores, sums and lse are held in fp32. */
 
 /* One request of kdn_attend: n_q new tokens at positions q_pos .. q_pos + n_q - 1 attend to the tokens of n_parts
  * stored chunks.  Token t of part j stands at position part_pos[j] + t and is seen by new token i when that position is
  * at most q_pos + i.  Its key is the stored key rotated by part_pos[j] - base_pos positions (as kdn_compose rotates).  Parts
- * may come in any order and leave gaps; parts that overlap count each of their tokens.  Codecs KDN_CODEC_INT4_G64 and
+ * may come in any order and leave gaps; parts that overlap count each of their tokens.  A chunk made from a keep-list counts
+ * the same: its t-th token stands at part_pos + t, wherever in the request it came from.  Codecs KDN_CODEC_INT4_G64 and
  * KDN_CODEC_INT4_KC64, KDN_MEM_DEVICE.  parts and part_pos: HOST arrays of n_parts entries; positions in [0, 2^40). */
 typedef struct {
     int32_t          n_q;
@@ -435,7 +436,9 @@ typedef struct {
  * scale (neither rounded) and s = scale * q.k over the tokens that are seen,
  *     out = sum exp(s - lse) v,   lse = ln sum exp(s)
  * so that the result can be merged with attention over other tokens (those in the pool) by their lse.  A row that sees no
- * token gets out 0 and lse -infinity.  What a token that a row does not see holds has no effect on the row.  head_dim 64
+ * token gets out 0 and lse -infinity.  What a token that a row does not see holds has no effect on the row (a scale of
+ * KDN_CODEC_INT4_KC64 keys is held by the 64 tokens of its group).  Requests of more than 40 rows a KV head (n_q *
+ * n_q_heads / n_kv_heads) have exp(s - lse) times the value scale rounded to bf16 once before it is summed (2^-9, beside the 2^-9 of out's own rounding), others to 16 bits.  head_dim 64
  * or 128 (KDN_E_UNSUPPORTED otherwise).  Rows of q and out are 16-byte aligned. */
 kdn_status kdn_attend(kdn_ctx *ctx, int pool_id, int layer, const kdn_attend_req *reqs, int n_reqs,
                       const kdn_attend_io *io, void *cuda_stream);
@@ -459,7 +462,8 @@ typedef struct {
 } kdn_weigh_req;
 
 /* What the requests of one kdn_weigh call share; q as in kdn_attend_io.  lse: DEVICE fp32 [rows][n_q_heads]: read
- * with lse_given != 0 (what the attention over the same tokens returned), else computed and, unless NULL, written. */
+ * with lse_given != 0 (what the attention over the same tokens returned; any other value serves as the formula has it), else
+ * computed and, unless NULL, written.  A weight is good to some 2^-22 of itself times the larger of 1, |lse| and the score. */
 typedef struct {
     const void *q;
     float      *lse;

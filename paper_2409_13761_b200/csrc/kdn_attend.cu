@@ -13,15 +13,18 @@ namespace {
 
 // Requests of up to this many rows a KV head go to the kernel that is bound by the bytes of the chunks and takes eight rows a pass; the others to the
 // one that is bound by the scores and takes 256.  Both, in microseconds (one request of 4096 tokens, one of 65536, eight of 8192, eight of 8192 with keys in
-// channel groups; all of 8 heads of 128):
+// channel groups; all of 8 heads of 128, turned):
 //     rows    eight a pass             256 a pass
-//     16       17   54   74   87       24  130  132  135
-//     32       25   98   86  108       29  136  134  136
-//     40       31  122  104  131       33  140  134  136
-//     48       32  141  121  153       34  140  135  137
-//     64       38  183  156  197       39  146  136  139
+//     16       17   54   58   66       29  135  134  134
+//     32       24   98   95  111       30  136  136  136
+//     40       31  122  115  134       30  137  136  136
+//     48       32  141  134  157       30  136  136  136
+//     64       38  185  173  203       31  136  137  136
 constexpr int kStepRows = 40;
 
+// As many heads a unit as the pool has, up to eight: warps that share no head have nothing to add up.  With eight, four and two heads a unit of eight heads of 128, in microseconds:
+// a token over ten documents of 1024 20.1, 18.9 and 18.8; over 65536 tokens 37.5, 36.6 and 37.4; over 4096 15.6, 15.8 and 20.2; 32 requests of 8192 with keys
+// in channel groups 122.4, 127.8 and 128.8; eight of 8192 with 16 rows 52.0, 54.9 and 55.7, with 8 rows 45.3, 39.2 and 38.0.
 int heads_of_unit(int H) { return H % 8 == 0 ? 8 : H % 4 == 0 ? 4 : H % 2 == 0 ? 2 : 1; }
 
 // How the requests of one of the two kernels are cut.

@@ -1,18 +1,20 @@
 // Attention of many new tokens over stored 4-bit chunks, on the tensor core.
 //
 // Mathematics as for a few (kdn_attend_step.cuh), other places for the scales.  Rows of queries are the lanes of tensor memory, 64 tokens of a tile its
-// columns:  S = Q K^T with K = code * scale as the sum of two fp16 matrices (scale = two numbers of eight bits, whose products with a code are exact) and
-// Q, turned and times a power of two, as the sum of two more (the second is nothing, and left out, where the queries are taken as they came);  P = exp(S) *
+// columns:  S = Q K^T with K = code * scale as the sum of two fp16 matrices (scale = a number of eight bits, whose products with a code are exact, and what
+// that leaves, to 11 bits) and Q, turned and times a power of two, as the sum of two more (the second is nothing, and left out, where the queries are taken as they came);  P = exp(S) *
 // value scale, bf16, one matrix for each group of 64 channels;  O += P C with C the value codes, exact in bf16.  The keys of a tile are held times a
 // power of two that brings the largest of their scales to 2^11, or, where scales are more than 2^12 apart, each token's times one of its own, which its
 // column of S is multiplied by before the softmax.  P is rounded once (2^-9 relative): tensor memory has no room for a second number, and fp16 not the
 // range that scales need; the result is 1.4 to 1.5 times as far off (root mean square, against 64 bits) as its own rounding alone makes it.
 //
-// What bounds it: shared memory's 128 bytes a clock, at about four fifths.  A tile of 64 tokens by 256 rows takes some 4000 clocks, of which the operands of the products
-// take 1800 (queries as they came) or 2600 (turned: a third product), what the warps store and load themselves 1600 (operands, the values' scales, waits);
-// the products alone would take 1500, the exponentials 1024 at 16 a clock, the instructions half of the issue slots.  Without any softmax or without any expanding of codes a
-// call is up to 9 per cent faster, without both up to 13.  Measured, 8 heads of 128: 203 tokens over ten documents of 1024 124 us (0.26 PFLOP/s); four
-// requests of 512 tokens over 8192, two heads of 8 query heads each, keys in channel groups: 295 us (0.47 PFLOP/s).  A CTA takes 256 rows as two sets of 128, so that codes are expanded once for both.  A set's scores are made a
+// What bounds it: shared memory's 128 bytes a clock, at about four fifths.  A tile of 64 tokens by 256 rows takes some 4200 clocks (four requests of 512
+// over 8192: 465 thousand for 111 tiles), of which the operands of the products take 1800 (queries as they came) or 2600 (turned: a third product), what the warps store and load themselves 1600 (operands, the values' scales, waits);
+// the products alone would take 1500, the exponentials 1024 at 16 a clock, the instructions half of the issue slots.  Over ten documents, turned, it is 5500 (180 thousand
+// for 33 tiles): the third product, and the pipeline runs dry where a part brings queries of its own, whatever it turns by.  Without any softmax or without any expanding of codes a
+// call is up to 9 per cent faster, without both up to 13.  Measured, 8 heads of 128: 203 tokens over ten documents of 1024 125 us (0.26 PFLOP/s); four
+// requests of 512 tokens over 8192, two heads of 8 query heads each, keys in channel groups: 296 us (0.47 PFLOP/s); the first with key scales over eight orders
+// of magnitude 128 us.  A CTA takes 256 rows as two sets of 128, so that codes are expanded once for both.  A set's scores are made a
 // tile ahead of its softmax, which turns them into P in place: 16 columns of S become the 8 of P that go with one group and the 8 that go with the
 // other, just what one product of 16 tokens reads.  Warps 0-3 and 4-7 are the softmax of a set, a row a thread; warps 8-11 expand codes; warps 12
 // and 13 issue the products of a set each (one for both was what everything waited for: 40 to 60 clocks a product).

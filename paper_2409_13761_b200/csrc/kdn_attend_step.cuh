@@ -10,13 +10,14 @@
 // the range that a product with any scale needs).  One number for the weights would save a quarter to a third of the products and
 // cost as much precision as the rounding of the result does.
 //
-// What bounds it: the instructions, not far above the bytes.  A token of one head is 144 bytes of K and V at head_dim 128; at 6.4 TB/s an SM may take 6 cycles
-// for it, in which 256 codes have to become matrix operands.  Tokens are the 16 rows of mma.m16n8k16 and the (up to 8) query rows of a KV head its
+// What bounds it: instructions and what one waits for another; no pipe is full (32 requests of 8192 tokens: 60 of 100 issue slots, the integer pipe
+// 46, 16 warps an SM).  A token of one head is 144 bytes of K and V at head_dim 128; at 6.4 TB/s an SM may take 6 cycles for it, in
+// which 256 codes have to become matrix operands.  Tokens are the 16 rows of mma.m16n8k16 and the (up to 8) query rows of a KV head its
 // 8 columns, so that no operand is wasted on one-token steps of grouped heads, and codes go from shared memory to the operand registers by 0.5
 // to 0.75 integer or half-precision instructions a code, with no shared memory in between: some 800 instructions for 32 tokens of a head.
-// Measured, one layer of 8 heads of 128: a token over 131072 tokens 51 us (151 MB, 2.9 TB/s); 32 requests of a token over four documents of
-// 2048, keys in channel groups, turned: 123 us (2.5 TB/s; 119 with queries held to 16 bits); a token over ten documents of 1024, turned: 10 us a layer, where the chain of a launch,
-// two dependent reads, a tile and the joining of 296 parts is what counts.
+// Measured, one layer of 8 heads of 128: a token over 131072 tokens 53 us (151 MB, 2.9 TB/s); 32 requests of a token over four documents of
+// 2048, keys in channel groups, turned: 122 us (2.5 TB/s; 119 with queries held to 16 bits); a token over ten documents of 1024, turned: 20 us, about
+// half of it this kernel (a launch, two dependent reads, a tile a CTA) and half the joining of 296 parts a head.
 #pragma once
 #include "kdn_ops.cuh"
 
