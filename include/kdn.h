@@ -399,7 +399,8 @@ kdn_status kdn_compose_select(kdn_ctx *ctx, int pool_id, const kdn_compose_req *
  * graphs that may run at the same time were captured with workspaces of their own).  Queries, outputs, weights and
  * workspaces lie on the context's device.  Outputs overlap neither inputs nor one another.  A request or chunk has up to
  * 2^28 tokens, and kdn_evict's as many rows (KDN_E_UNSUPPORTED).  A call that is refused enqueues nothing.  NaN that a row reads (in its query, in a scale or a key that
- * it sees) makes that row's results NaN, and with kdn_weigh what the row adds.  Scores, sums and lse are held in fp32. */
+ * it sees) makes that row's results NaN, and with kdn_weigh what the row adds.  Scores, sums and lse are held in fp32;
+ * a row with scores past its range is NaN too. */
 
 /* One request of kdn_attend: n_q new tokens at positions q_pos .. q_pos + n_q - 1 attend to the tokens of n_parts
  * stored chunks.  Token t of part j stands at position part_pos[j] + t and is seen by new token i when that position is

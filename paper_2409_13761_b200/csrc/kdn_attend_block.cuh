@@ -302,8 +302,8 @@ __global__ void __launch_bounds__(kBlockThreads, 1) kdn_attend_block_kernel(cons
             if (all) maxima(std::true_type{});
             else maxima(std::false_type{});
             top *= scale;
-            // huge scores are multiplied and rounded before the reference is taken off
-            if (__any_sync(0xffffffffu, fabsf(top) > kHugeScore && fabsf(top) != INFINITY)) {
+            // huge scores are multiplied and rounded before the reference is taken off (a row of scores past fp32's range is NaN then)
+            if (__any_sync(0xffffffffu, fabsf(top) > kHugeScore && top != -INFINITY)) {
                 const float by = fabsf(top) > kHugeScore ? scale : 1.0f;
 #pragma unroll 1
                 for (int c0 = 0; c0 < kBlockTile; c0 += 16) {

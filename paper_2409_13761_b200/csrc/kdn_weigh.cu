@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) kdn_weigh_many_kernel(const __g
                                 m = top;
                             }
                             float by = L.scale;
-                            if (__any_sync(0xffffffffu, fabsf(top) > kHugeScore && fabsf(top) != INFINITY) && fabsf(top) > kHugeScore) {
+                            if (__any_sync(0xffffffffu, fabsf(top) > kHugeScore && top != -INFINITY) && fabsf(top) > kHugeScore) {
                                 by = 1.0f;
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * L.scale);

@@ -291,6 +291,26 @@ def test_attend_with_huge_scores(gain, codec, n_q):
         dev.close()
 
 
+@pytest.mark.parametrize("codec", [G64, KC64])
+@pytest.mark.parametrize("n_q", [1, 11, 70])
+def test_scores_past_the_range_of_fp32(codec, n_q):
+    """A row whose scores are infinite in 32 bits is NaN, not one that saw nothing; the others keep their bits."""
+    dev = make_attend(2, 128)
+    try:
+        rng = np.random.default_rng(7)
+        c = AttendCase(dev, rng, [(n_q, 400, [(200, codec, 7, 0), (150, codec, 0, 200)])], 4).call().check()
+        want, want_lse = c.out.clone(), c.lse.clone()
+        c.q[n_q // 2, 5] = torch.sign(c.q[n_q // 2, 5].float()) * 1e38
+        c.call()
+        assert dev.sync() == 0
+        assert torch.isnan(c.out[n_q // 2, 5]).all() and torch.isnan(c.lse[n_q // 2, 5])
+        rest = torch.ones_like(c.lse, dtype=torch.bool)
+        rest[n_q // 2, 5] = False
+        assert torch.equal(c.out[rest], want[rest]) and torch.equal(c.lse[rest], want_lse[rest])
+    finally:
+        dev.close()
+
+
 # ------------------------------------------------------------------------------- NaN that is seen --
 
 @pytest.mark.parametrize("codec", [G64, KC64])
